@@ -700,8 +700,10 @@ maps_status maps_kv_read(const void* cache, int32_t num_blocks, int32_t block_si
  * Position t lies in block table[b][t / block_size], place t mod block_size.
  * out is dense [T][q_heads][D] of q's type; lse ([T][q_heads], float) may be
  * NULL.  max_q is the caller's bound on a request's query tokens.
- * Scores and sums are held in 32 bits; probabilities are rounded to the
- * precision of q's type before they meet the values.  Keys and values that a
+ * Scores and sums are held in 32 bits.  Probabilities are rounded to 16 bits
+ * or more before they meet the values, with MAPS_BF16 to 8 where more than 16
+ * columns (queries of a request times heads that share a KV head) lie side by
+ * side.  Keys and values that a
  * query does not see have no influence on it, NaN among them.  The rows of a
  * request with an error are left as they were.
  * workspace: maps_kv_attend_workspace_size(B, T, q_heads, heads, dim, max_q)

@@ -17,8 +17,9 @@
 //                 operand; the page keeps V in groups of 4 tokens so that one
 //                 load gives lane (g, r) the same 4 keys and D / 16 channels,
 //                 and conversion by the token's scale plus one byte
-//                 permutation gives V^T's.  With f16 the probabilities go in
-//                 as two bf16 pieces.
+//                 permutation gives V^T's.  The probabilities go in as two
+//                 bf16 pieces, 16 bits or more; from 32 columns of bf16 queries
+//                 on, as one (kPieces below).
 // The softmax keeps one running maximum a column, moved only when a score
 // exceeds it by 2^8: sums stay far inside 32 bits, and most tiles need no
 // exchange between lanes.
@@ -145,6 +146,12 @@ struct Wave {
     static constexpr int kCols = 16 * NT;
     static constexpr int kSteps = D / 32;                             // 32-channel steps of the scores
     static constexpr int kTerms = F16 ? 2 : 1;                        // bf16 pieces of a query
+    // bf16 pieces of a probability.  One leaves an error against 64 bits that is 1.1 to 1.35 times that of rounding the
+    // output alone (2.0e-3 .. 2.3e-3 of the outputs' norm against 1.6e-3 .. 1.8e-3), two leave no more than that.  With 16
+    // columns, where memory bounds, two take 125.0 us instead of 123.9 (256 requests), 39.4 instead of 39.1 (one of
+    // 131,072 positions); in prompts, which the products bound, 1,128 instead of 906 (2,048 query tokens of two
+    // requests): there one is enough for outputs of the same 8 bits.
+    static constexpr int kPieces = F16 || NT == 1 ? 2 : 1;
     static constexpr int kChunks = D > 128 ? D / 128 : 1;              // scales of a lane's channels of a key
     static constexpr int kOut = D / 16;                               // 16-channel steps of the output
     static constexpr int kBytes = D / 32;                             // V bytes of a lane and token
@@ -316,7 +323,7 @@ struct Wave {
     __device__ __forceinline__ void step(Tile& w, int32_t tile, float c, const Pages& next, bool edge) {
         const int32_t t0 = tile * kTile;
         uint32_t nan = 0;          // V scales that are NaN, a bit a half and token, of this lane's keys
-        uint32_t p[NT][F16 ? 2 : 1][4];
+        uint32_t p[NT][kPieces][4];
         float t[NT][8];            // raw scores; the powers of two are c times them
         auto highest = [&](int nt) {
             float top = t[nt][0];
@@ -386,7 +393,7 @@ struct Wave {
             for (int i = 0; i < 4; ++i) {
                 const kv::bf16x2 hi = {__bf16(e[2 * i]), __bf16(e[2 * i + 1])};
                 p[nt][0][i] = __builtin_bit_cast(uint32_t, hi);
-                if constexpr (F16) {
+                if constexpr (kPieces == 2) {
                     const kv::bf16x2 lo = rest(e[2 * i], e[2 * i + 1], hi);
                     p[nt][1][i] = __builtin_bit_cast(uint32_t, lo);
                 }
@@ -437,7 +444,7 @@ struct Wave {
 #pragma unroll
                 for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-                    for (int k = 0; k < (F16 ? 2 : 1); ++k) {
+                    for (int k = 0; k < kPieces; ++k) {
                         const u32x4 pb = {p[nt][k][0], p[nt][k][1], p[nt][k][2], p[nt][k][3]};
                         acc[nt][2 * b + half] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
                             __builtin_bit_cast(bf16x8, va), __builtin_bit_cast(bf16x8, pb), acc[nt][2 * b + half], 0, 0, 0);
