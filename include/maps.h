@@ -705,7 +705,9 @@ maps_status maps_kv_read(const void* cache, int32_t num_blocks, int32_t block_si
  * columns (queries of a request times heads that share a KV head) lie side by
  * side.  Keys and values that a
  * query does not see have no influence on it, NaN among them.  The rows of a
- * request with an error are left as they were.
+ * request whose lens or tok_off are in error, and rows before tok_off[0], are
+ * left as they were; where table gives an id out of range, the rows that see a
+ * position of that block become NaN, out and lse, and no others.
  * workspace: maps_kv_attend_workspace_size(B, T, q_heads, heads, dim, max_q)
  * bytes.  dev_err bits: NEG_LEN (lens < 0), SEG_OFFSETS (tok_off decreasing,
  * outside [0, T], or a request with more than max_q queries), BLOCK_TABLE (a

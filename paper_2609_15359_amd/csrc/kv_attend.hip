@@ -160,6 +160,7 @@ struct Wave {
     struct Tile {
         uint32_t k[2][kSteps];
         uint32_t ks[2][kChunks];
+        uint32_t none[2];          // scale bits of a half whose block does not exist: NaN, else 0
         uint32_t v[2][kBytes];
         uint32_t vs[2];
     };
@@ -264,6 +265,7 @@ struct Wave {
     // Where the halves' keys and key scales lie; the values' are a.v_skip behind them.
     struct Pages {
         const char *code[2], *scale[2];
+        uint32_t none[2];
     };
     __device__ Pages pages_of(int32_t tile, Ids ids) {
         Pages p;
@@ -271,9 +273,12 @@ struct Wave {
         for (int s = 0; s < 2; ++s) {
             const int32_t t = tile * kTile + (s && tile * kTile + 16 < len ? 16 : 0);
             uint32_t id = uint32_t(ids.id[s]);
+            p.none[s] = 0;
             if (id >= uint32_t(a.num_blocks)) {
+                // block 0 is read in its place, as keys that are NaN: so is what a query that sees them gets
                 bad = true;
                 id = 0;
+                p.none[s] = kv::kScaleNan << 23;
             }
             const uint32_t at = uint32_t(t) & ((1u << a.shift) - 1);   // a multiple of 16
             const char* page = pages + uint64_t(id) * a.block;
@@ -286,6 +291,7 @@ struct Wave {
     __device__ void load_keys(Tile& w, const Pages& p) {
 #pragma unroll
         for (int s = 0; s < 2; ++s) {
+            w.none[s] = p.none[s];
             if constexpr (D == 64) {                                   // 16 channels of the half's key r
                 const kv::u32x2 x = *reinterpret_cast<const kv::u32x2*>(p.code[s] + uint32_t(r * (D / 2) + g * 8));
                 w.k[s][0] = x[0];
@@ -339,7 +345,7 @@ struct Wave {
             for (int nt = 0; nt < NT; ++nt) z[nt] = f32x4{0, 0, 0, 0};
 #pragma unroll
             for (int i = 0; i < kSteps; ++i) {
-                const float scale = kv::scale_value(w.ks[s][D == 64 ? 0 : i / 4]);
+                const float scale = __uint_as_float(w.ks[s][D == 64 ? 0 : i / 4] << 23 | w.none[s]);
                 u32x4 k;
                 unrolled<4>([&](auto byte) {
                     constexpr int b = decltype(byte)::value;
