@@ -634,7 +634,8 @@ maps_status maps_project_order(int32_t D, const int64_t* seg_off, int64_t n_tota
  * blocks stay held and are used again.
  * dev_err bits: NEG_LEN, BLOCK_TABLE (held outside [0, max_blocks], a slot
  * that would need more than max_blocks or has more tokens than its blocks
- * take, an id or the ring out of range), SEG_OFFSETS (more than T tokens).
+ * take, an id or the ring out of range), SEG_OFFSETS (more than T tokens: no
+ * slot is granted, so that no block is taken for a token without an entry).
  * Host errors: NULL, SIZE (B outside [1, MAPS_MAX_STEP_REQUESTS], max_blocks,
  * block_size or num_blocks < 1, B max_blocks > INT32_MAX, T outside
  * [0, INT32_MAX]), HIP.

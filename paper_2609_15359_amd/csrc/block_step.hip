@@ -118,7 +118,9 @@ __global__ __launch_bounds__(NT, 4) void block_step_kernel(StepArgs a) {
     }
     const bool room = uint32_t(returned) <= N - count;   // else the ring has been given blocks twice
     if (!room) err |= MAPS_ERR_BLOCK_TABLE;
-    if (total > a.T) err |= MAPS_ERR_SEG_OFFSETS;
+    // a token past T would leave the table without the block that it starts: nothing grows then, and no block is lost
+    const bool listed = total <= a.T;
+    if (!listed) err |= MAPS_ERR_SEG_OFFSETS;
     auto sat = [](int64_t x) { return int32_t(x < INT32_MAX ? x : INT32_MAX); };   // T is no more
     auto at = [&](uint32_t i) { return i >= N ? i - N : i; };                       // i < 2 N
     const bool first_wg = blockIdx.x == 0;
@@ -127,7 +129,7 @@ __global__ __launch_bounds__(NT, 4) void block_step_kernel(StepArgs a) {
         const int32_t before = int32_t(blocks), mine = need[b] & int32_t(~kFlag), grow = off[b];
         const int64_t step = moves(b);
         const uint32_t ended = own[b] & kFlag;
-        const bool granted = need[b] >= 0 && (mine == 0 || uint32_t(before) + uint32_t(mine) <= count);
+        const bool granted = listed && need[b] >= 0 && (mine == 0 || uint32_t(before) + uint32_t(mine) <= count);
         if (first_wg) {
             a.granted[b] = granted;
             a.lens_out[b] = int32_t(len[b]) + (granted ? grow : 0);

@@ -112,6 +112,27 @@ def test_value_errors():
     assert err == ["SEG_OFFSETS"]
 
 
+@pytest.mark.parametrize("B,short", [(20, 1), (20, 30), (300, 1), (300, 500)])
+def test_a_total_that_is_too_small_takes_no_block(B, short):
+    """No slot is granted, blocks of finished requests come back all the same, and every block is in a row or in the ring
+    once."""
+    rng = np.random.RandomState(B + short)
+    s = _state(rng, B, 6, 16, 200 * B // 20, grow_hi=40)
+    s["grow"] = np.minimum(s["grow"], 6 * 16 - np.where(s["done"], 0, s["lens"])).astype(np.int32)
+    N, T = len(s["ring"]), int(s["grow"].sum()) - short
+    got, err = _run(s, 16, T)
+    assert err == ["SEG_OFFSETS"]
+    zero = {**s, "grow": np.zeros_like(s["grow"])}
+    want = ref.block_step(zero["grow"], s["table"], s["held"], s["lens"], s["ring"], s["ring_pos"], 16, T, s["done"])
+    for k in ("table", "ring", "lens", "held", "ring_pos"):
+        assert np.array_equal(got[k].astype(np.int64), np.asarray(want[k], np.int64)), k
+    assert not got["granted"].any() and (got["slots"] == -1).all()
+    assert np.array_equal(got["tok_off"], np.concatenate([[0], np.cumsum(s["grow"].astype(np.int64))]))
+    used = np.concatenate([got["table"][b, :got["held"][b]] for b in range(B)])
+    free = got["ring"][(got["ring_pos"][0] + np.arange(got["ring_pos"][1])) % N]
+    assert sorted(np.concatenate([used, free]).tolist()) == list(range(N))
+
+
 def test_tables_from_step_to_step():
     """BlockTables over 30 steps of requests that come, grow, shrink and end, against the reference on the host."""
     import torch
