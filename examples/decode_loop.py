@@ -72,12 +72,12 @@ def serve(model: Model, prompts, new_tokens: int, drafts: int, cache_bytes: int,
     no_drafts = torch.empty((B, 0), dtype=torch.int32, device=dev)
 
     def step(tokens, grow, total, max_q, done=None):
-        """Feeds `total` tokens, grow[b] of them to request b; the attention's output and where each request starts."""
+        """Feeds `total` tokens, grow[b] of them to request b; the attention's output, and what the tables gave."""
         s = tables.step(grow, total, done)
         maps.kv_append(cache, model.k[tokens], model.v[tokens], s.slots, tables.dev_err)
         out, _ = maps.kv_attend(cache, model.q[tokens], tables.table, tables.lens, s.tok_off, max_q, model.scale,
-                                dev_err=tables.dev_err)
-        return out, s.tok_off
+                                dev_err=tables.dev_err, granted=s.granted)
+        return out, s
 
     def verify(target, drafted, n_draft):
         u = torch.rand(drafted.shape, generator=g, device=dev)
@@ -87,8 +87,8 @@ def serve(model: Model, prompts, new_tokens: int, drafts: int, cache_bytes: int,
     # prompts: the last token of each gives the first answer's distribution
     lens = torch.tensor([len(p) for p in prompts], dtype=torch.int32, device=dev)
     flat = torch.tensor([x for p in prompts for x in p], device=dev)
-    out, off = step(flat, lens, flat.numel(), max(map(len, prompts)))
-    target = model.probabilities(out[off[1:] - 1])[:, None]
+    out, s = step(flat, lens, flat.numel(), max(map(len, prompts)))
+    target = model.probabilities(out[s.tok_off[1:] - 1])[:, None]
     first, _ = verify(target, no_drafts, torch.zeros(B, dtype=torch.int32, device=dev))
     answers = first.tolist()                                                             # [B][1]
 
@@ -106,16 +106,17 @@ def serve(model: Model, prompts, new_tokens: int, drafts: int, cache_bytes: int,
         grow = torch.where(alive, K + 1, 0).to(torch.int32)
         done = (~alive).to(torch.uint8) & (1 - ended)                                    # give their blocks back, once
         ended |= done
-        out, _ = step(fed, grow, fed.numel(), K + 1, done)
+        out, s = step(fed, grow, fed.numel(), K + 1, done)
         target = torch.zeros((B, K + 1, V), device=dev)
         target[rows] = model.probabilities(out).unflatten(0, (-1, K + 1))
-        n_draft = torch.where(alive, K, -1).to(torch.int32)
+        fed_to = alive & (s.granted != 0)     # (a refused request tries again; this cache has room for all)
+        n_draft = torch.where(fed_to, K, -1).to(torch.int32)
         tokens, accepted = verify(target, chain[:, 1:].contiguous(), n_draft)
         # the rejected drafts' places are used again
-        tables.lens -= torch.where(alive, K - accepted, 0).to(torch.int32)
+        tables.lens -= torch.where(fed_to, K - accepted, 0).to(torch.int32)
         steps += 1
         for b, (n, row) in enumerate(zip(accepted.tolist(), tokens.tolist())):
-            if not live[b]:
+            if n < 0:
                 continue
             for x, y in zip(answers[b][-1:] + row[:n], row[:n + 1]):
                 follows[x] = y

@@ -632,6 +632,11 @@ maps_status maps_project_order(int32_t D, const int64_t* seg_off, int64_t n_tota
  * the rows of finished requests, so a call whose `done` slots do not grow can
  * be repeated.  A later call may set lens[b] lower (rejected drafts): the
  * blocks stay held and are used again.
+ * A pool that is short raises no error bit.  A refused slot's new tokens are in
+ * no cache, so that what follows in the step has to leave them out: negative
+ * slots are skipped by maps_kv_append; maps_kv_attend is given 0 in the place of
+ * the slot's lens (else its rows would be queries of the last tokens that are
+ * cached), maps_verify_drafts -1 as its n_draft.
  * dev_err bits: NEG_LEN, BLOCK_TABLE (held outside [0, max_blocks], a slot
  * that would need more than max_blocks or has more tokens than its blocks
  * take, an id or the ring out of range), SEG_OFFSETS (more than T tokens: no
@@ -697,7 +702,8 @@ maps_status maps_kv_read(const void* cache, int32_t num_blocks, int32_t block_si
  * s_t = scale <q, k_t> over the seen t,
  *   out = sum_t exp(s_t) v_t / sum_t exp(s_t),   lse = log sum_t exp(s_t);
  * a query that sees nothing (p < 0) gets out = 0 and lse = -infinity, as do
- * the rows of q from tok_off[B] up to T.
+ * the rows of q from tok_off[B] up to T.  The query tokens have to be in the
+ * cache: a slot that maps_block_step refused is given with lens 0.
  * Position t lies in block table[b][t / block_size], place t mod block_size.
  * out is dense [T][q_heads][D] of q's type; lse ([T][q_heads], float) may be
  * NULL.  max_q is the caller's bound on a request's query tokens.

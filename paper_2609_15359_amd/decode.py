@@ -63,7 +63,7 @@ class BlockStep:
     lens: torch.Tensor        # [B] int32, tokens after the step
     held: torch.Tensor        # [B] int32, blocks after the step
     ring_pos: torch.Tensor    # [2] int32, the ring's front and count after the step
-    granted: torch.Tensor     # [B] uint8
+    granted: torch.Tensor     # [B] uint8, 0: refused, its new tokens have no slots (kv_attend takes this array)
     dev_err: torch.Tensor
 
 
@@ -231,11 +231,13 @@ def kv_attend_workspace_bytes(B: int, T: int, q_heads: int, heads: int, dim: int
 
 
 def kv_attend(cache: KVCache, q, table, lens, tok_off, max_q: int, scale: float, window: int = 0,
-              want_lse: bool = False, dev_err=None, workspace=None, out=None, lse=None):
+              want_lse: bool = False, dev_err=None, workspace=None, out=None, lse=None, granted=None):
     """Attention of the step's query tokens q [T, q_heads, dim] (request b's
     are tok_off[b] .. tok_off[b+1]-1, the last of its lens[b] tokens) over the
     cache, causal, with a sliding window of `window` positions if that is not
-    0.  Returns (out [T, q_heads, dim], lse [T, q_heads] or None)."""
+    0.  granted: the step's, for a pool that can be short: a refused request's
+    new tokens are not in the cache, and its rows get out = 0, lse = -infinity.
+    Returns (out [T, q_heads, dim], lse [T, q_heads] or None)."""
     _rows(q, (torch.bfloat16, torch.float16), (None, None, cache.dim), "q")
     T, Hq, dim = q.shape
     heads = cache.heads
@@ -245,6 +247,10 @@ def kv_attend(cache: KVCache, q, table, lens, tok_off, max_q: int, scale: float,
         raise MapsError(f"table must be [B, max_blocks] with B = {B} (got {tuple(table.shape)})")
     if _dense(tok_off, torch.int64, "tok_off").numel() != B + 1:
         raise MapsError(f"tok_off must have {B + 1} entries")
+    if granted is not None:
+        if _dense(granted, torch.uint8, "granted").numel() != B:
+            raise MapsError(f"granted must have {B} entries")
+        lens = lens * (granted != 0)
     if out is None:
         out = q.new_empty((T, Hq, dim))
     elif _dense(out, q.dtype, "out").shape != q.shape:

@@ -1,0 +1,93 @@
+"""The calls of a step one after the other, where a slot gets no blocks: what the step refuses stays out of the cache, the
+attention and the verification, and goes in with the step that grants it."""
+import numpy as np
+import pytest
+
+from tests import decode_ref as ref
+
+pytestmark = pytest.mark.gpu
+
+
+def _fits(out, lse, cache, q, table, lens, off, scale):
+    """Against the reference in 64 bits, with the bounds of one rounding to bf16 of the output (2^-8) and, of wide
+    stretches, of the probabilities (2^-8); scores of a few units, whose error of 2 e < 2^-12 is asserted."""
+    want, want_lse, A, mag = ref.attend(cache.data.cpu().numpy(), q.double().cpu().numpy(), table.cpu().numpy(),
+                                        lens, off, scale, 0, cache.block_size, cache.dim)
+    assert 2 * scale * (cache.dim * 2.0 ** -23 * mag[..., 0] + 2.0 ** -20 * mag[..., 1]).max() < 2.0 ** -12
+    out, lse = out.double().cpu().numpy(), lse.double().cpu().numpy()
+    assert np.array_equal(np.isneginf(lse), np.isneginf(want_lse)) and not out[np.isneginf(want_lse)].any()
+    assert (np.abs(out - want) <= 2.0 ** -8 * np.abs(want) + (2.0 ** -8 + 2.0 ** -11) * A).all()
+    fine = np.isfinite(want_lse)
+    assert (np.abs(lse[fine] - want_lse[fine]) <= 2.0 ** -12 + 2.0 ** -19 * (1 + np.abs(want_lse[fine]))).all()
+
+
+@pytest.mark.parametrize("K", [0, 3])
+def test_a_refused_request_waits_for_its_blocks(K):
+    """Requests 1 and 2 need a block each, the pool has one: 2 is refused.  Its rows see nothing and its verification is
+    skipped; when request 0 has ended, the same tokens are granted."""
+    import torch
+
+    import paper_2609_15359_amd as maps
+    rng = np.random.RandomState(4)
+    B, H, G, D, S, V = 4, 2, 3, 64, 16, 50
+    first = np.array([S, S, 2 * S, 5], np.int32)
+    t = maps.BlockTables(B, 4, 6, S)
+    cache = maps.KVCache.empty(6, H, D, S)
+    cache.data.fill_(0xFF)
+
+    def dev(x, dtype):
+        return torch.from_numpy(np.ascontiguousarray(x)).to(dtype).cuda()
+
+    def step(grow, done=None):
+        grow = np.asarray(grow, np.int32)
+        T = int(grow.sum())
+        r = t.step(dev(grow, torch.int32), T, None if done is None else dev(done, torch.uint8))
+        k, v = (dev(rng.standard_normal((T, H, D)), torch.bfloat16) for _ in range(2))
+        q = dev(rng.standard_normal((T, H * G, D)), torch.bfloat16)
+        maps.kv_append(cache, k, v, r.slots, t.dev_err)
+        return r, q, maps.kv_attend(cache, q, t.table, t.lens, r.tok_off, int(grow.max()), D ** -0.5, want_lse=True,
+                                    dev_err=t.dev_err, granted=r.granted)
+
+    def check(r, q, out, lse):
+        _fits(out, lse, cache, q, t.table, (t.lens * r.granted).tolist(), r.tok_off.tolist(), D ** -0.5)
+
+    r, q, (out, lse) = step(first)
+    assert r.granted.tolist() == [1] * B
+    check(r, q, out, lse)
+    bytes_before = cache.data.clone()
+    refused = t.table[2, :2].tolist()
+    grow = np.full(B, K + 1)
+    grow[0] = 0
+    r, q, (out, lse) = step(grow)
+    assert r.granted.tolist() == [1, 1, 0, 1] and t.lens.tolist() == [S, S + K + 1, 2 * S, 5 + K + 1]
+    check(r, q, out, lse)
+    a, b = r.tok_off[2:4].tolist()
+    assert (r.slots[a:b] == -1).all() and not out[a:b].any() and torch.isneginf(lse[a:b]).all()
+    assert torch.equal(cache.data[refused], bytes_before[refused])
+    n_draft = torch.where(r.granted != 0, K, -1).to(torch.int32)
+    p = torch.softmax(torch.randn((B, K + 1, V), device="cuda"), -1)
+    tokens, accepted = maps.verify_drafts(p, torch.zeros((B, K), dtype=torch.int32, device="cuda"), n_draft,
+                                          torch.rand((B, K), device="cuda"), torch.ones((B, V), device="cuda"))
+    assert accepted[2] == -1 and (tokens[2] == -1).all() and (accepted[[0, 1, 3]] >= 0).all()
+    t.lens -= torch.where(r.granted != 0, K - accepted, 0).to(torch.int32) * (torch.arange(B, device="cuda") > 0)
+    lens = t.lens.tolist()
+    t.step(torch.zeros(B, dtype=torch.int32, device="cuda"), 0, dev([1, 0, 0, 0], torch.uint8))
+    assert t.lens.tolist() == [0] + lens[1:]
+    r, q, (out, lse) = step([0, 0, K + 1, 0])
+    assert r.granted.tolist() == [1] * B and t.lens.tolist() == [0, lens[1], 2 * S + K + 1, lens[3]]
+    check(r, q, out, lse)
+    maps.check_errors(t.dev_err)
+
+
+def test_granted_is_checked():
+    import torch
+
+    import paper_2609_15359_amd as maps
+    cache = maps.KVCache.empty(2, 1, 64, 16)
+    q = torch.zeros((2, 1, 64), dtype=torch.bfloat16, device="cuda")
+    i32 = dict(dtype=torch.int32, device="cuda")
+    args = (cache, q, torch.zeros((2, 1), **i32), torch.ones(2, **i32), torch.arange(3, device="cuda"), 1, 1.0)
+    with pytest.raises(maps.MapsError, match="granted must have 2"):
+        maps.kv_attend(*args, granted=torch.ones(3, dtype=torch.uint8, device="cuda"))
+    with pytest.raises(TypeError, match="granted"):
+        maps.kv_attend(*args, granted=torch.ones(2, **i32))
