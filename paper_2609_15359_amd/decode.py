@@ -38,6 +38,19 @@ def _current(t):
     return _raw_stream(t.get_device()) if _raw_stream is not None else _stream(t.device)
 
 
+def _apart(written, others):
+    """Raises unless every dense tensor of `written` shares no byte with the others of it and with `others`."""
+    spans = sorted((t.data_ptr(), t.data_ptr() + t.numel() * t.element_size(), w)
+                   for ts, w in ((written, True), (others, False)) for t in ts if t.numel())
+    last = last_written = 0                  # ends of the spans so far
+    for start, end, w in spans:
+        if start < (last if w else last_written):
+            raise MapsError("out's arrays must not overlap each other or the ones that the call reads")
+        last = max(last, end)
+        if w:
+            last_written = max(last_written, end)
+
+
 @lru_cache(maxsize=4096)
 def _size(name, *sizes):
     """A size query of the library, which depends on its arguments alone."""
@@ -92,12 +105,16 @@ def block_step(grow, table, held, lens, ring, ring_pos, block_size: int, total: 
         out = BlockStep(slots=new(T, dtype=torch.int64), tok_off=new(B + 1, dtype=torch.int64), lens=new(B), held=new(B),
                         ring_pos=new(2), granted=new(B, dtype=torch.uint8), dev_err=err)
     else:
-        _dense(out.slots, torch.int64, "out.slots")
-        if out.slots.numel() != T or out.lens.numel() != B or out.held.numel() != B or out.tok_off.numel() != B + 1:
-            raise MapsError("out was made for another step's sizes")
-        for x, y in ((out.lens, lens), (out.held, held), (out.ring_pos, ring_pos)):
-            if x.data_ptr() == y.data_ptr():
-                raise MapsError("out's arrays must not be the ones that the call reads")
+        given = (("slots", torch.int64, T), ("tok_off", torch.int64, B + 1), ("lens", torch.int32, B),
+                 ("held", torch.int32, B), ("ring_pos", torch.int32, 2), ("granted", torch.uint8, B))
+        for name, dtype, n in given:
+            t = _dense(getattr(out, name), dtype, "out." + name)
+            if t.numel() != n:
+                raise MapsError(f"out was made for another step's sizes: {name} must have {n} entries")
+            if t.get_device() != grow.get_device():
+                raise MapsError(f"out.{name} must be on {grow.device} (got {t.device})")
+        _apart([getattr(out, name) for name, _, _ in given], [grow, lens, held, table, ring, ring_pos, err] +
+               ([] if done is None else [done]))
         out.dev_err = err
     st = library().maps_block_step(B, table.shape[1], int(block_size), N, _at(done), _at(grow), _at(lens),
                                    _at(held), _at(table), _at(ring), _at(ring_pos), _at(out.lens),

@@ -133,6 +133,49 @@ def test_a_total_that_is_too_small_takes_no_block(B, short):
     assert sorted(np.concatenate([used, free]).tolist()) == list(range(N))
 
 
+def test_arrays_to_write_into():
+    """A result of an earlier call takes the next one's values; whatever else could be written past or while it is read
+    is refused before anything is launched."""
+    import dataclasses
+
+    import torch
+
+    import paper_2609_15359_amd as maps
+    rng = np.random.RandomState(13)
+    s = _state(rng, 30, 5, 16, 60, done_share=0.0, grow_hi=9)
+    s["grow"] = np.minimum(s["grow"], 5 * 16 - s["lens"]).astype(np.int32)
+    T, B = int(s["grow"].sum()), 30
+    d = {k: torch.from_numpy(np.ascontiguousarray(v)).cuda() for k, v in s.items() if k != "done"}
+    first = maps.block_step(block_size=16, total=T, **d)
+    def empty(n, dtype=torch.int32):
+        return torch.empty(n, dtype=dtype, device="cuda")
+    blank = maps.BlockStep(slots=empty(T, torch.int64), tok_off=empty(B + 1, torch.int64), lens=empty(B), held=empty(B),
+                           ring_pos=empty(2), granted=empty(B, torch.uint8), dev_err=first.dev_err)
+    again = maps.block_step(block_size=16, total=T, out=blank, **d)
+    assert again is blank
+    for name in ("slots", "tok_off", "lens", "held", "ring_pos", "granted"):
+        assert torch.equal(getattr(again, name), getattr(first, name)), name
+    before = {k: v.clone() for k, v in d.items()}
+    both = empty(2 * B - 1)
+    for wrong, error, what in (
+            (dict(slots=empty(T + 1, torch.int64)), maps.MapsError, "slots"), (dict(tok_off=empty(B, torch.int64)), maps.MapsError, "tok_off"),
+            (dict(lens=empty(B - 1)), maps.MapsError, "lens"), (dict(held=empty(B + 1)), maps.MapsError, "held"),
+            (dict(ring_pos=empty(1)), maps.MapsError, "ring_pos"), (dict(granted=empty(B - 1, torch.uint8)), maps.MapsError, "granted"),
+            (dict(tok_off=empty(B + 1)), TypeError, "tok_off"), (dict(lens=empty(B, torch.int64)), TypeError, "lens"),
+            (dict(held=empty(B, torch.uint8)), TypeError, "held"), (dict(ring_pos=empty(2, torch.int64)), TypeError, "ring_pos"),
+            (dict(granted=empty(B)), TypeError, "granted"), (dict(held=empty(2 * B)[::2]), maps.MapsError, "contiguous"),
+            (dict(granted=torch.empty(B, dtype=torch.uint8)), maps.MapsError, "device tensor"),
+            (dict(held=d["lens"]), maps.MapsError, "overlap"), (dict(lens=d["grow"]), maps.MapsError, "overlap"),
+            (dict(lens=d["lens"]), maps.MapsError, "overlap"), (dict(held=d["ring"][5:5 + B]), maps.MapsError, "overlap"),
+            (dict(lens=d["table"].flatten()[-B:]), maps.MapsError, "overlap"),
+            (dict(ring_pos=d["ring_pos"]), maps.MapsError, "overlap"),
+            (dict(lens=both[:B], held=both[B - 1:]), maps.MapsError, "overlap")):
+        with pytest.raises(error, match=what):
+            maps.block_step(block_size=16, total=T, out=dataclasses.replace(blank, **wrong), **d)
+    torch.cuda.synchronize()
+    assert all(torch.equal(d[k], before[k]) for k in d)
+
+
 def test_tables_from_step_to_step():
     """BlockTables over 30 steps of requests that come, grow, shrink and end, against the reference on the host."""
     import torch
