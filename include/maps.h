@@ -675,8 +675,9 @@ maps_status maps_block_step(int32_t B, int32_t max_blocks, int32_t block_size, i
  * magnitude as a float (2 = the field below which a code's value would leave
  * the normal numbers), and the nearest E2M1 number of x 2^(127 - s), ties to
  * the even code, at most 6; 32 channels with an infinity or NaN among them
- * become NaN.  Negative slots are skipped; equal slots in one call leave
- * either token's values.
+ * become NaN.  Negative slots are skipped.  The others have to differ within a
+ * call, as those of maps_block_step do: a slot that is given twice is left with
+ * unspecified values, whose codes and scales may come from either token.
  * maps_kv_read gives the values that the cache stands for at T slots, rounded
  * to `dtype`, as dense [T][heads][D] arrays; a negative slot gives zeros.
  * dev_err bits: SLOT (a slot >= num_blocks * S: skipped, or read as zeros).

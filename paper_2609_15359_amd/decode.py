@@ -210,7 +210,7 @@ def _rows(t, dtypes, shape, name):
 
 def kv_append(cache: KVCache, k, v, slots, dev_err=None):
     """Quantises T tokens' keys and values ([T, heads, dim]) into the cache at
-    `slots` (negative: skipped).  Returns dev_err."""
+    `slots` (negative: skipped; the others must differ).  Returns dev_err."""
     T = _dense(slots, torch.int64, "slots").numel()
     _rows(k, tuple(_TYPES), (T, cache.heads, cache.dim), "k")
     _rows(v, (k.dtype,), (T, cache.heads, cache.dim), "v")
