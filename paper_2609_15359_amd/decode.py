@@ -311,6 +311,8 @@ def verify_drafts(target, draft_tokens, n_draft, u, noise, draft=None, dev_err=N
     tokens, accepted = out if out is not None else (n_draft.new_empty((B, K + 1)), n_draft.new_empty(B))
     if _dense(tokens, torch.int32, "tokens").shape != (B, K + 1) or _dense(accepted, torch.int32, "accepted").numel() != B:
         raise MapsError("out must be tokens [B, K + 1] and accepted [B]")
+    if B == 0:
+        return tokens, accepted
     err = new_error_word(target.device) if dev_err is None else dev_err
     ws = _scratch(_size("maps_verify_drafts_workspace_size", B, V), target, workspace)
     st = library().maps_verify_drafts(B, K, V, _at(target), target.stride(0), target.stride(1), _at(draft),

@@ -133,6 +133,18 @@ def test_views():
     assert np.array_equal(out.cpu().numpy(), want) and np.array_equal(accepted.cpu().numpy(), want_accepted)
 
 
+@pytest.mark.parametrize("with_draft", [True, False])
+def test_no_requests(with_draft):
+    import torch
+
+    import paper_2609_15359_amd as maps
+    def empty(*shape, dtype=torch.float32):
+        return torch.empty(shape, dtype=dtype, device="cuda")
+    tokens, accepted = maps.verify_drafts(empty(0, 4, 50), empty(0, 3, dtype=torch.int32), empty(0, dtype=torch.int32),
+                                          empty(0, 3), empty(0, 50), draft=empty(0, 3, 50) if with_draft else None)
+    assert tokens.shape == (0, 4) and accepted.shape == (0,) and tokens.dtype == accepted.dtype == torch.int32
+
+
 def test_value_errors():
     *x, ty = _inputs(6, 6, 2, 50, "float32")
     x[3][:] = 2
