@@ -722,7 +722,8 @@ maps_status maps_kv_read(const void* cache, int32_t num_blocks, int32_t block_si
  * length of more than max_blocks blocks, an id out of range).
  * Host errors: NULL, SIZE (B outside [1, MAPS_MAX_STEP_REQUESTS], T outside
  * [0, INT32_MAX], q_heads not a multiple of heads, window < 0, max_q < 1, ..),
- * TYPE, ALIGN (cache, q, out and workspace to 16 bytes, q's strides to 8 elements),
+ * TYPE, ALIGN (cache, q, out and workspace to 16 bytes, q's strides to 8 elements
+ * where there is more than one token or head),
  * WORKSPACE, HIP.
  */
 size_t maps_kv_attend_workspace_size(int32_t B, int64_t T, int32_t q_heads, int32_t heads, int32_t dim,

@@ -893,8 +893,8 @@ extern "C" maps_status maps_kv_attend(const void* cache, int32_t num_blocks, int
         return MAPS_E_SIZE;
     if (dtype != MAPS_BF16 && dtype != MAPS_F16) return MAPS_E_TYPE;
     if (!cache || !table || !lens || !tok_off || !dev_err || (T > 0 && (!q || !out))) return MAPS_E_NULL;
-    if (!aligned(cache, 16) || !aligned(q, 16) || !aligned(out, 16) || !aligned(workspace, 16) || q_stride_t % 8 ||
-        q_stride_h % 8)
+    if (!aligned(cache, 16) || !aligned(q, 16) || !aligned(out, 16) || !aligned(workspace, 16) ||
+        (T > 1 && q_stride_t % 8) || (q_heads > 1 && q_stride_h % 8))   // (one row needs no stride)
         return MAPS_E_ALIGN;
     if (T == 0) return MAPS_OK;
     if (max_q > T) max_q = int32_t(T);

@@ -85,6 +85,19 @@ def test_attend(lib):
     assert attend(T=0) == 0
 
 
+def test_attend_needs_no_stride_of_one_row(lib):
+    """Strides of axes of size 1 are free (what is refused is the workspace, which comes behind the alignment), and a
+    workspace that is missing or a byte short is refused; the tables are wide enough for all workgroups."""
+    def attend(T, Hq, st, sh, ws=FAKE, short=1):
+        need = lib.maps_kv_attend_workspace_size(3, T, Hq, 1, 128, 4)
+        return lib.maps_kv_attend(FAKE, 4096, 16, 1, 128, FAKE, 0, T, Hq, st, sh, FAKE, 3, 2**20, FAKE, FAKE, 4, 0.1, 0, FAKE,
+                                  None, FAKE, ws, need - short, None)
+
+    assert attend(1, 8, 1001, 128) == -4 and attend(1, 1, 3, 5) == -4 and attend(4, 1, 128, 129) == -4
+    assert attend(2, 8, 1001, 128) == -9 and attend(1, 8, 1024, 129) == -9 and attend(4, 1, 130, 129) == -9
+    assert attend(4, 8, 1024, 128) == -4 and attend(4, 8, 1024, 128, None, 0) == -1
+
+
 def test_verify(lib):
     def verify(B=3, K=2, V=100, target=FAKE, ty=2, tokens=FAKE, n=FAKE, u=FAKE, noise=FAKE, out=FAKE, acc=FAKE, err=FAKE,
                ws=FAKE, short=0):
