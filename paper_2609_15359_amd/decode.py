@@ -52,9 +52,14 @@ def _apart(written, others):
 
 
 @lru_cache(maxsize=4096)
-def _size(name, *sizes):
-    """A size query of the library, which depends on its arguments alone."""
+def _size(name, device, *sizes):
+    """A size query of the library, which depends on its arguments and, if `device` is not None, on the current device's
+    compute units."""
     return int(getattr(library(), name)(*sizes))
+
+
+def _current_device():
+    return torch.cuda.current_device() if torch.cuda.is_initialized() else -1
 
 
 def _scratch(nbytes, t, given):
@@ -168,7 +173,7 @@ class KVCache:
     def page_bytes(block_size: int, dim: int) -> int:
         """Bytes of one block of one KV head; block_size is a power of two in
         [16, 256], dim 64, 128 or 256."""
-        n = _size("maps_kv_page_bytes", int(block_size), int(dim))
+        n = _size("maps_kv_page_bytes", None, int(block_size), int(dim))
         if n == 0:
             raise MapsError(f"no page of block_size = {block_size}, dim = {dim}")
         return n
@@ -244,7 +249,9 @@ def kv_read(cache: KVCache, slots, dtype=torch.bfloat16, dev_err=None, out=None)
 
 
 def kv_attend_workspace_bytes(B: int, T: int, q_heads: int, heads: int, dim: int, max_q: int) -> int:
-    return _size("maps_kv_attend_workspace_size", int(B), int(T), int(q_heads), int(heads), int(dim), int(max_q))
+    """Bytes that kv_attend's workspace needs on the current device."""
+    return _size("maps_kv_attend_workspace_size", _current_device(), int(B), int(T), int(q_heads), int(heads), int(dim),
+                 int(max_q))
 
 
 def kv_attend(cache: KVCache, q, table, lens, tok_off, max_q: int, scale: float, window: int = 0,
@@ -314,7 +321,7 @@ def verify_drafts(target, draft_tokens, n_draft, u, noise, draft=None, dev_err=N
     if B == 0:
         return tokens, accepted
     err = new_error_word(target.device) if dev_err is None else dev_err
-    ws = _scratch(_size("maps_verify_drafts_workspace_size", B, V), target, workspace)
+    ws = _scratch(_size("maps_verify_drafts_workspace_size", None, B, V), target, workspace)
     st = library().maps_verify_drafts(B, K, V, _at(target), target.stride(0), target.stride(1), _at(draft),
                                 0 if draft is None else draft.stride(0), 0 if draft is None else draft.stride(1),
                                 _TYPES[target.dtype], _at(draft_tokens), _at(n_draft), _at(u), _at(noise),

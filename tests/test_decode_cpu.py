@@ -115,6 +115,28 @@ def test_verify(lib):
     assert lib.maps_verify_drafts_workspace_size(0, 5) == 0 and lib.maps_verify_drafts_workspace_size(5, 0) == 0
 
 
+def test_workspace_sizes_follow_the_device(monkeypatch):
+    """Attention's workspace depends on the device's compute units: a size that one device gave is no other's."""
+    import torch
+
+    class Library:
+        device = 0
+
+        def maps_kv_attend_workspace_size(self, *sizes):
+            return 1000 * (self.device + 1)
+
+    lib = Library()
+    monkeypatch.setattr(maps.decode, "library", lambda: lib)
+    monkeypatch.setattr(torch.cuda, "is_initialized", lambda: True)
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: lib.device)
+    maps.decode._size.cache_clear()
+    try:
+        for lib.device in (0, 1, 0, 3):
+            assert maps.decode.kv_attend_workspace_bytes(3, 5, 8, 2, 128, 1) == 1000 * (lib.device + 1)
+    finally:
+        maps.decode._size.cache_clear()
+
+
 def test_binding_refuses_host_tensors_and_shapes():
     import torch
     i32 = torch.zeros(4, dtype=torch.int32)
