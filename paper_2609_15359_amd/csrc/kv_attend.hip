@@ -515,8 +515,9 @@ struct Wave {
         }
         Ids ids = load_ids(clip(first + 1));
         load_queries(rq, p);
-        // (a scale of zero would make NaN of the infinities that mark unseen positions)
-        const float c = a.scale == 0.0f ? 1e-37f : fabsf(a.scale) * kLog2e;
+        // a scale of zero would make NaN of the infinities that mark unseen positions: 2^-149 stands for it, which leaves
+        // 2^-21 of the largest finite product
+        const float c = a.scale == 0.0f ? 0x1p-149f : fabsf(a.scale) * kLog2e;
         for (int32_t tile = first; tile < end; ++tile) {
             const bool edge = tile * kTile + kTile - 1 > lo || (a.window && tile * kTile <= hi - a.window);
             const Pages to = pages_of(clip(tile + 1), ids);
