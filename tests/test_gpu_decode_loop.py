@@ -57,3 +57,29 @@ def test_a_cache_that_is_too_small_is_refused():
     from examples.decode_loop import Model, serve
     with pytest.raises(ValueError, match="too small"):
         serve(Model.random(), [[1, 2, 3]], 40, 2, 1 << 10)
+
+
+@pytest.mark.parametrize("drafts", [0, 1, 4])
+def test_accepted_drafts_save_steps(drafts):
+    """A model whose token x is always followed by x + 1 mod 5: a query is twice its token's key (entries of 1 and -1), so
+    that attention gives that token's value, and the projection takes it to the next token.  Once the drafter has seen the
+    five pairs, after at most five steps, every draft is accepted and a step gives drafts + 1 tokens."""
+    import torch
+
+    from examples.decode_loop import Model, serve
+    V, H, G, D = 5, 2, 2, 64
+    g = torch.Generator().manual_seed(5)
+    def signs():
+        return 2.0 * torch.randint(0, 2, (V, H, D), generator=g) - 1.0
+    k, v = signs(), signs()
+    proj = v.roll(1, 0).repeat_interleave(G, 1).flatten(1).T                  # column y: the value of token y - 1
+    bf16 = dict(device="cuda", dtype=torch.bfloat16)
+    model = Model(q=(2 * k).repeat_interleave(G, 1).to(**bf16), k=k.to(**bf16), v=v.to(**bf16),
+                  proj=proj.contiguous().cuda(), temperature=1.0)
+    prompts = [[0], [3, 1, 1, 4], [2] * 33]
+    answers, steps = serve(model, prompts, 40, drafts, 1 << 19)
+    assert answers == [[(p[-1] + 1 + i) % V for i in range(40)] for p in prompts]
+    if drafts:
+        assert steps <= 1 + V + -(-39 // (drafts + 1))
+    else:
+        assert steps == 40
