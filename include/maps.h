@@ -631,7 +631,11 @@ maps_status maps_project_order(int32_t D, const int64_t* seg_off, int64_t n_tota
  * two of each and swaps them); nothing that the call reads is overwritten but
  * the rows of finished requests, so a call whose `done` slots do not grow can
  * be repeated.  A later call may set lens[b] lower (rejected drafts): the
- * blocks stay held and are used again.
+ * blocks stay held and are used again.  Such a slot holds more than the
+ * ceil((p + g) / S) blocks that maps_rsc_state counts for its tokens, so that
+ * B_free exceeds the ring's count and requests can be dispatched against blocks
+ * that a step then refuses; with g = held[b] * S - p for each slot, B_free is
+ * the ring's count.
  * A pool that is short raises no error bit.  A refused slot's new tokens are in
  * no cache, so that what follows in the step has to leave them out: negative
  * slots are skipped by maps_kv_append; maps_kv_attend is given 0 in the place of

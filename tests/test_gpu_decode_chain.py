@@ -79,6 +79,33 @@ def test_a_refused_request_waits_for_its_blocks(K):
     maps.check_errors(t.dev_err)
 
 
+def test_free_blocks_as_placement_counts_them():
+    """Blocks that rejected drafts leave held are missing from the ring but not from B_free by tokens; by held blocks, B_free
+    is the ring's count."""
+    import torch
+
+    import paper_2609_15359_amd as maps
+    S, N, K = 16, 40, 20
+    prompt = torch.tensor([16, 30, 1, 12], dtype=torch.int32, device="cuda")
+    t = maps.BlockTables(4, 8, N, S)
+    t.step(prompt, int(prompt.sum()))
+    t.step(torch.full_like(prompt, K + 1), 4 * (K + 1))
+    t.lens -= K                                                     # every draft is rejected
+    free = int(t.ring_pos[1])
+    assert free == N - (3 + 4 + 2 + 3)                              # 37, 51, 22, 33 tokens
+
+    def b_free(generated):
+        offsets = torch.tensor([0, 4], device="cuda")
+        capacity = torch.tensor([N * S], dtype=torch.int32, device="cuda")
+        b, _, _, err = maps.rsc_state(offsets, prompt, generated.contiguous(), torch.full_like(prompt, 60), capacity, S)
+        maps.check_errors(err)
+        return int(b)
+
+    assert b_free(t.lens - prompt) == N - (2 + 2 + 1 + 1) > free    # 17, 31, 2, 13 tokens
+    assert b_free(t.held * S - prompt) == free
+    maps.check_errors(t.dev_err)
+
+
 def test_granted_is_checked():
     import torch
 
