@@ -26,8 +26,6 @@ inline bool dim_ok(int D) { return D == 64 || D == 128 || D == 256; }
 inline int type_bytes(int32_t dtype) { return dtype == MAPS_F32 ? 4 : 2; }
 
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
-typedef short s16x2 __attribute__((ext_vector_type(2)));
-typedef unsigned short u16x2 __attribute__((ext_vector_type(2)));
 typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
 typedef float f32x2 __attribute__((ext_vector_type(2)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));

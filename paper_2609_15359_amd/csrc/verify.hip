@@ -90,7 +90,7 @@ __global__ __launch_bounds__(kVerifyNT) void race_kernel(VerifyArgs a) {
     const int b = blockIdx.x / a.pieces, piece = blockIdx.x % a.pieces;
     const uint32_t from = uint32_t(piece) * kPiece;         // (rows of nearly 2^31 entries: sums below stay inside 32 bits)
     const uint32_t end = uint32_t(a.V) - from < kPiece ? uint32_t(a.V) : from + kPiece;
-    // the noise is the same row whatever is accepted: on its way while the drafts are compared
+    // (the noise is the same row whatever is accepted, but loading it ahead of the comparisons costs wavefronts)
     const float* noise = a.noise + b * a.noise_stride;
     constexpr int kRounds = kPiece / (4 * kVerifyNT);
     uint32_t err = 0;

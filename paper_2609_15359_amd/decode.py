@@ -175,7 +175,8 @@ class KVCache:
         [16, 256], dim 64, 128 or 256."""
         n = _size("maps_kv_page_bytes", None, int(block_size), int(dim))
         if n == 0:
-            raise MapsError(f"no page of block_size = {block_size}, dim = {dim}")
+            raise MapsError(f"no page of block_size = {block_size}, dim = {dim}: block_size is a power of two in "
+                            f"[16, {MAX_CACHE_BLOCK}], dim 64, 128 or 256")
         return n
 
     @classmethod
