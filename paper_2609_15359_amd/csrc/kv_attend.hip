@@ -33,15 +33,16 @@
 // first among the wavefronts of a workgroup and then by a second launch, both
 // in the order of the line: the same inputs give the same bits.
 //
-// Measured, us a call (both launches): 256 requests of 128 .. 8,192 tokens, 8
-// KV heads of 128, 4 query heads each, bf16: 122 = 4.5 TB/s of cache, bound by
-// memory (a large copy runs at 4.9); one request of 131,072 tokens: 44, of
-// which the join is 8; up to 5 drafted tokens a request and 6 heads a KV head
-// in f16 with a window: 77, vector instructions 40% of the SIMDs' cycles
-// (conversions, and a softmax whose columns are half empty), products 26%, the
-// rest waits that two wavefronts a SIMD do not cover; 2,048 query tokens of two
-// requests of 10,000 and 14,000: 946 = 761 TFLOP/s, vector instructions 63%,
-// products 33% (a large matrix product of the library reaches 1,215).
+// Measured, us a call (both launches; cards differ by 5%): 256 requests of 128
+// .. 8,192 tokens, 8 KV heads of 128, 4 query heads each, bf16: 123 = 4.4 TB/s
+// of cache, bound by memory (a large copy runs at 4.8 .. 4.9); one request of
+// 131,072 tokens: 44, of which the join is 8; up to 5 drafted tokens a request
+// and 6 heads a KV head in f16 with a window: 77, vector instructions 34% of
+// the SIMDs' cycles (conversions, and a softmax whose columns are half empty),
+// products 26%, the rest waits that two wavefronts a SIMD do not cover; 2,048
+// query tokens of two requests of 9,742 and 13,777: 913 .. 970 = 743 .. 789
+// TFLOP/s, vector instructions 56%, products 33% (a large matrix product of the
+// library reaches 1,190 .. 1,215).
 #include "kv_page.hpp"
 
 namespace maps {
@@ -825,10 +826,14 @@ __global__ __launch_bounds__(kJoinNT) void kv_join_kernel(AttendArgs a) {
 
 // 16-column steps of a wavefront.  More of them share the keys' and values' conversions, until the sums leave the 256
 // registers of half the file and are moved between its halves around every branch:
-//   64 channels: as few as hold the longest request's columns, at most 4 (a prompt chunk: 132 us, with 2 147);
-//   128: at most 2 (2,048 query tokens of two requests, f16 / bf16: 1,387 / 1,054 us, with 4 2,038 / 1,133);
-//   256: 1 up to 32 columns (20 requests of 5 drafts and 6 heads: 43 / 41 us, with 2 50 / 46), 2 from there (700 query
-//   tokens of two requests: 300 / 239 us, with 1 294 / 271).
+// Measured in bf16 / f16, us, on prompts (the last tokens of two requests of 9,742 and 13,777, 4 heads a KV head) and
+// chunks (100 tokens of 16 requests of 500 .. 4,000):
+//   64 channels: as few as hold the longest request's columns, at most 4 (1,024 tokens 276 / 399, with 2 377 / 460, although
+//   14 registers spill in f16; chunks 69 / 91, with 2 73 / 86);
+//   128: at most 2 (2,048 tokens 909 / 1,258, with 4 1,105 / 2,016, with 1 1,384 / 1,596; chunks 95 / 120, with 4 127 / 213);
+//   256: 2 (700 tokens 437 / 542, with 1 546 / 570; chunks 121 / 144, with 1 124 / 129), but 1 up to 32 columns: where
+//   requests have fewer drafts than the longest, 2 costs up to 18% more (20 requests of up to 16,000 tokens, 1 to 5 drafts and 6
+//   heads: 55 / 57, with 2 60 / 67); where all have as many, it is from 13% less (5 each: 71 / 75, with 2 62 / 70) to 8% more.
 int col_tiles(int32_t G, int32_t max_q, int32_t D) {
     const int64_t cols = int64_t(G) * max_q;
     return cols <= (D == 256 ? 32 : 16) ? 1 : cols <= 32 || D > 64 ? 2 : 4;

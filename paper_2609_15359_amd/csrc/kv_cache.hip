@@ -5,8 +5,9 @@
 // share a scale are neighbours and exchange their largest magnitude by lane
 // moves; the codes come from the conversion instruction, which rounds x / 2^e
 // to the nearest E2M1 number, ties to the even code, and stops at 6.  Memory
-// bound: 16-bit values in and 17/32 bytes a value out.  32,768 tokens of 8 heads
-// of 128 channels in bf16: appended and read back in 79 us = 4.3 TB/s.
+// bound: values in and 17/32 bytes a value out.  32,768 tokens of 8 heads of 128
+// channels: appended in 35 us from 16-bit types (4.9 TB/s) and in 57 from f32
+// (5.3), read back in 31 (5.4) and 79 (3.9).
 #include "kv_page.hpp"
 
 namespace maps {

@@ -7,10 +7,10 @@
 // complemented index: the lowest index wins ties), and a second launch takes
 // the best piece.  A request's K comparisons are repeated by each of its
 // pieces.  Memory bound: one row of the target, one of the noise and, after a
-// refusal, one of the drafts.  256 requests with 4 drafts over 131,072 entries
-// in f32: 77 us = 4.4 TB/s (single entries a load: 96; 8 entries a thread: 127;
-// the noise loaded ahead of the drafts' comparison: 162, its registers leave
-// half of the wavefronts).
+// refusal, one of the drafts.  256 requests with 4 drafts over 131,072 entries,
+// 179 of them refused: 76 us in f32 = 4.8 TB/s (single entries a load: 96; 8
+// entries a thread: 127; the noise loaded ahead of the drafts' comparison: 162,
+// its registers leave half of the wavefronts), 54 in 16-bit types = 4.6.
 #include "kv_page.hpp"
 
 namespace maps {
