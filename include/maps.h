@@ -713,9 +713,9 @@ maps_status maps_kv_read(const void* cache, int32_t num_blocks, int32_t block_si
  * out is dense [T][q_heads][D] of q's type; lse ([T][q_heads], float) may be
  * NULL.  max_q is the caller's bound on a request's query tokens.
  * Scores and sums are held in 32 bits.  Probabilities are rounded to 16 bits
- * or more before they meet the values, with MAPS_BF16 to 8 where more than 16
- * columns (queries of a request times heads that share a KV head) lie side by
- * side.  Keys and values that a
+ * or more before they meet the values, with MAPS_BF16 to as few as 8 where a
+ * request can have more than 16 columns (max_q times the heads that share a KV
+ * head).  Keys and values that a
  * query does not see have no influence on it, NaN among them.  The rows of a
  * request whose lens or tok_off are in error, and rows before tok_off[0], are
  * left as they were; where table gives an id out of range, the rows that see a
@@ -727,8 +727,7 @@ maps_status maps_kv_read(const void* cache, int32_t num_blocks, int32_t block_si
  * Host errors: NULL, SIZE (B outside [1, MAPS_MAX_STEP_REQUESTS], T outside
  * [0, INT32_MAX], q_heads not a multiple of heads, window < 0, max_q < 1, ..),
  * TYPE, ALIGN (cache, q, out and workspace to 16 bytes, q's strides to 8 elements
- * where there is more than one token or head),
- * WORKSPACE, HIP.
+ * where there is more than one token or head), WORKSPACE, HIP.
  */
 size_t maps_kv_attend_workspace_size(int32_t B, int64_t T, int32_t q_heads, int32_t heads, int32_t dim,
                                      int32_t max_q);
